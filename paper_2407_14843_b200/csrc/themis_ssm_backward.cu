@@ -60,10 +60,13 @@ template <typename T, int LPC> struct Shape {
     static constexpr int RESIDENT = LPC == 4 || LPC == 8 ? 2 : 3;   // blocks of a multiprocessor
     // The inputs of a chunk as they are; 16-bit ones twice, the next chunk's arriving meanwhile (two
     // buffers of 32-bit ones would leave room for one block to a multiprocessor).
-    struct Raw {
-        T x[kChunk + 3][CT];                                     // the three times before the chunk first
-        T dt[kChunk][CT], z[kChunk][CT], dy[kChunk][CT];
-        T b[kChunk][NP], c[kChunk][NP];
+    struct Raw {                                                 // (every array on the 16 bytes of a copy)
+        alignas(16) T x[kChunk + 3][CT];                         // the three times before the chunk first
+        alignas(16) T dt[kChunk][CT];
+        alignas(16) T z[kChunk][CT];
+        alignas(16) T dy[kChunk][CT];
+        alignas(16) T b[kChunk][NP];
+        alignas(16) T c[kChunk][NP];
     };
     static constexpr int BUFS = sizeof(T) == 4 ? 1 : 2;
     static constexpr size_t BYTES = FLOATS * sizeof(float) + BUFS * sizeof(Raw);
@@ -77,12 +80,14 @@ template <typename T, int NPT, int LPC> struct LocalShape {
     static constexpr int PAIRS = CT / 2;
     static constexpr int E = kChunk * PAIRS / THREADS;
     struct Tile {
-        struct Raw {
-            T dt[kChunk][CT], z[kChunk][CT], dy[kChunk][CT];
-            T c[kChunk][NP];
+        struct Raw {                                             // (every array on the 16 bytes of a copy)
+            alignas(16) T dt[kChunk][CT];
+            alignas(16) T z[kChunk][CT];
+            alignas(16) T dy[kChunk][CT];
+            alignas(16) T c[kChunk][NP];
         } raw[2];
-        float2 se[kChunk][CT];                                   // s_t and e_t
-        float c[kChunk][NP];
+        alignas(16) float2 se[kChunk][CT];                       // s_t and e_t
+        alignas(16) float c[kChunk][NP];
     };
 };
 
@@ -162,7 +167,12 @@ __global__ __launch_bounds__(128, sizeof(T) == 4 ? 3 : 4) void ssm_adjoint_local
     using S = LocalShape<T, NPT, LPC>;
     constexpr int CT = S::CT, NP = S::NP, E = S::E, THREADS = S::THREADS;
     extern __shared__ __align__(16) float smem[];
-    auto &s = *reinterpret_cast<typename S::Tile *>(smem);
+    using Tile = typename S::Tile;
+    using Raw = typename Tile::Raw;
+    static_assert(sizeof(Raw) % 16 == 0 && offsetof(Raw, dt) % 16 == 0 && offsetof(Raw, z) % 16 == 0 && offsetof(Raw, dy) % 16 == 0 &&
+                      offsetof(Raw, c) % 16 == 0 && offsetof(Tile, raw) % 16 == 0 && offsetof(Tile, se) % 16 == 0 && offsetof(Tile, c) % 16 == 0,
+                  "rows are copied and read 16 bytes at a time");
+    auto &s = *reinterpret_cast<Tile *>(smem);
 
     const int D = p.pr.channels, N = p.pr.state, tid = threadIdx.x;
     const int b = blockIdx.x, split = blockIdx.z + 1;       // nothing needs the first part's share
@@ -302,7 +312,12 @@ __global__ __launch_bounds__(Shape<T, LPC>::THREADS, Shape<T, LPC>::RESIDENT) vo
     float *s_dA = take(S::SLOT);
     float(*s_carry)[CT] = reinterpret_cast<float(*)[CT]>(take(3 * CT));         // dc of the next chunk's first times
     float(*s_par)[CT] = reinterpret_cast<float(*)[CT]>(take(kPars * CT));
-    typename S::Raw *s_raw = reinterpret_cast<typename S::Raw *>(at_);
+    using Raw = typename S::Raw;
+    static_assert(sizeof(Raw) % 16 == 0 && offsetof(Raw, x) % 16 == 0 && offsetof(Raw, dt) % 16 == 0 && offsetof(Raw, z) % 16 == 0 &&
+                      offsetof(Raw, dy) % 16 == 0 && offsetof(Raw, b) % 16 == 0 && offsetof(Raw, c) % 16 == 0,
+                  "rows are copied and read 16 bytes at a time");
+    static_assert(CT % 4 == 0 && S::SLOT % 4 == 0 && NP % 4 == 0 && S::PARTS % 4 == 0 && S::FLOATS % 4 == 0, "so are the arrays before it");
+    Raw *s_raw = reinterpret_cast<Raw *>(at_);
 
     const int D = p.pr.channels, N = p.pr.state, W = p.pr.conv_width, L = p.pr.length, G = p.pr.groups;
     const int b = blockIdx.x, split = blockIdx.z, tid = threadIdx.x, lane = tid % 32, warp = tid / 32;
@@ -377,7 +392,7 @@ __global__ __launch_bounds__(Shape<T, LPC>::THREADS, Shape<T, LPC>::RESIDENT) vo
 #pragma unroll
         for (int i = 0; i < 4; ++i) h[i] = pack2(v[0][i], v[1][i]);
     };
-    auto fetch = [&](int t0, typename S::Raw &r) {
+    auto fetch = [&](int t0, Raw &r) {
         RowCopy<T, CT, kChunk + 3, THREADS>(xp, p.pr.x_time, nd, tid).run(&r.x[0][0], t0 - 3, len, tid);
         RowCopy<T, CT, kChunk, THREADS>(dtp, p.pr.dt_time, nd, tid).run(&r.dt[0][0], t0, len, tid);
         if (zp) RowCopy<T, CT, kChunk, THREADS>(zp, p.pr.z_time, nd, tid).run(&r.z[0][0], t0, len, tid);

@@ -29,17 +29,20 @@ template <typename T, int NPT, int LPC> struct Shape {
     static constexpr int NP = NPT * LPC;                 // states, padded (A = B = C = 0 beyond N)
 };
 
-// Shared memory of a block.  x, dt, B and C of the next tile arrive while this one is worked on.
+// Shared memory of a block.  x, dt, B and C of the next tile arrive while this one is worked on.  Every array
+// starts on the 16 bytes of an asynchronous copy, in both buffers (four 16-bit values of an unused C would
+// put the second buffer 8 bytes off).
 template <typename T, int NPT, int LPC, bool LOCAL> struct Tile {
     using S = Shape<T, NPT, LPC>;
     struct Raw {
-        T x[S::TT + 3][S::CT];                           // the three times before the tile first
-        T dt[S::TT][S::CT];
-        T b[S::TT][S::NP], c[LOCAL ? 1 : S::TT][S::NP];
+        alignas(16) T x[S::TT + 3][S::CT];               // the three times before the tile first
+        alignas(16) T dt[S::TT][S::CT];
+        alignas(16) T b[S::TT][S::NP];
+        alignas(16) T c[LOCAL ? 1 : S::TT][S::NP];
     } raw[2];
-    T z[LOCAL ? 1 : S::TT][S::CT];
-    float2 su[S::TT][S::CT];                             // s_t and u_t, then v_t
-    float bc[S::TT][2 * S::NP];
+    alignas(16) T z[LOCAL ? 1 : S::TT][S::CT];
+    alignas(16) float2 su[S::TT][S::CT];                 // s_t and u_t, then v_t
+    alignas(16) float bc[S::TT][2 * S::NP];
 };
 
 // blocks of a multiprocessor (registers)
@@ -53,7 +56,13 @@ __global__ __launch_bounds__(kThreads, kPlaces<T>) void ssm_scan_kernel(const Ss
     using S = Shape<T, NPT, LPC>;
     constexpr int CT = S::CT, E = S::E, TT = S::TT, NP = S::NP;
     extern __shared__ __align__(16) uint8_t smem[];
-    auto &s = *reinterpret_cast<Tile<T, NPT, LPC, LOCAL> *>(smem);
+    using Buffers = Tile<T, NPT, LPC, LOCAL>;
+    using Raw = typename Buffers::Raw;
+    static_assert(sizeof(Raw) % 16 == 0 && offsetof(Raw, x) % 16 == 0 && offsetof(Raw, dt) % 16 == 0 && offsetof(Raw, b) % 16 == 0 &&
+                      offsetof(Raw, c) % 16 == 0 && offsetof(Buffers, raw) % 16 == 0 && offsetof(Buffers, z) % 16 == 0 &&
+                      offsetof(Buffers, su) % 16 == 0 && offsetof(Buffers, bc) % 16 == 0,
+                  "rows are copied and read 16 bytes at a time");
+    auto &s = *reinterpret_cast<Buffers *>(smem);
 
     const int D = p.pr.channels, N = p.pr.state, W = p.pr.conv_width, L = p.pr.length;
     const int b = blockIdx.x, split = blockIdx.z, tid = threadIdx.x;

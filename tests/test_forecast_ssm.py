@@ -377,3 +377,50 @@ def test_refusals(F):
     with pytest.raises(F.ThemisError) as e:
         F.ssm_scan(**long, workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))
     assert e.value.code == F.E_WORKSPACE_TOO_SMALL
+
+
+# --- parts of several tiles ------------------------------------------------------------------------
+
+def parts_of(F, a, backward):
+    """Number of parts of the time axis, from the workspace that the call asks for."""
+    names = ("x", "dt", "A", "B", "C", "conv_weight", "conv_bias", "skip", "dt_bias", "z", "conv_state", "ssm_state", "lengths")
+    problem, _, N, W = F._ssm_args(**{k: a.get(k) for k in names}, step=False)
+    (rows, length, D), G = a["x"].shape, a["B"].shape[2]
+    tile = 128 if N <= 16 else 64 if N <= 32 else 16                # channels of a block of the gradients' kernel
+    def need(s):
+        sizes = [rows * s * D * N, rows * s * D] if s > 1 else []
+        if backward:
+            sizes += [rows * s * D * (N + 8), -(-(D // G) // tile) * rows * length * G * 2 * N]
+            sizes += [rows * s * (W - 1) * D] * 2 if s > 1 else []
+        return sum(-(-4 * v // 256) * 256 for v in sizes)
+    found = [s for s in range(1, -(-length // F.SSM_CHUNK) + 1) if need(s) == F.themis_ssm_workspace_bytes(problem, backward)]
+    assert len(found) == 1
+    return found[0]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16], ids=["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("state,views", [(1, False), (3, False), (4, False), (4, True), (8, False), (16, False), (16, True), (40, False)],
+                         ids=lambda v: str(v))
+def test_parts_of_several_tiles(F, state, views, dtype):
+    """Parts that take both input buffers, with rows that are copied 16 bytes at a time (contiguous inputs of 136
+    channels) and value by value (slices at an odd offset)."""
+    a = make(8, 2041, 136, state, dtype=dtype, seed=30 + state, views=views)
+    a["A"] = a["A"] * 0.02                   # long memories, so that the parts depend on each other
+    chunks = -(-2041 // F.SSM_CHUNK)
+    assert 2 <= parts_of(F, a, False) <= chunks // 4 and 2 <= parts_of(F, a, True) <= chunks // 2
+    dy = torch.randn(8, 2041, 136, device="cuda").to(dtype)
+    leaves = {k: a[k].detach().double().requires_grad_() for k in NAMES}
+    y, conv, h = R.scan(**{**a, **leaves})
+    ref = dict(zip((NAMES[k] for k in leaves), torch.autograd.grad(y, list(leaves.values()), dy.double())))
+    r = F.ssm_scan(**a, save=True)
+    got = F.ssm_scan_backward(dy, r.checkpoints, **a)
+    R.close(r.y, y.detach(), terms=512, what="y")
+    R.close(r.ssm_state, h.detach(), terms=512, what="state")
+    assert torch.equal(r.conv_state.double(), conv.detach())
+    for k in ref:
+        R.close(got[k], ref[k], terms=1024, what=k)
+    # rows that end inside a part, and before it
+    ragged = dict(a, lengths=torch.tensor([0, 1, 40, 700, 701, 1500, 2040, 2041], dtype=torch.int32, device="cuda"))
+    s = F.ssm_scan(**spoil(ragged), states=False)
+    for b, n in enumerate(ragged["lengths"].tolist()):
+        assert torch.equal(s.y[b, :n], r.y[b, :n]) and (s.y[b, n:] == 0).all()
