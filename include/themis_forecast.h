@@ -158,7 +158,9 @@ int themis_linear_workspace_bytes(const themis_linear_problem_t *problem, int ba
  *   d_y         T [M][N] out, contiguous
  *   d_pre       T [M][N] out, contiguous, or NULL: what the backward call of an activation needs
  *   d_status    int32 or NULL: THEMIS_STATUS_TIMEOUT is written to it if a bounded on-device wait
- *               expired (the result is then void); never written otherwise
+ *               expired (the result is then void); never written otherwise.  Any memory that the
+ *               device can write; in pinned host memory the host can poll it.  With NULL an
+ *               expired wait is not reported
  */
 int themis_linear_forward(const themis_linear_problem_t *problem, const void *d_x, const void *d_weight,
                           const float *d_bias, const void *d_residual, void *d_y, void *d_pre,

@@ -19,7 +19,7 @@ from typing import NamedTuple, Optional
 import torch
 
 from . import solver
-from .solver import E_INVALID_ARG, E_UNSUPPORTED_SIZE, E_WORKSPACE_TOO_SMALL, OK, ThemisError  # noqa: F401
+from .solver import E_INVALID_ARG, E_UNSUPPORTED_SIZE, E_WORKSPACE_TOO_SMALL, OK, STATUS_TIMEOUT, ThemisError  # noqa: F401
 
 DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
@@ -90,6 +90,42 @@ _lib = _bind(ctypes.CDLL(solver.LIB_PATH))
 def _check(rc: int, where: str) -> None:
     if rc != OK:
         raise ThemisError(rc, where)
+
+
+class WaitExpired(RuntimeError):
+    """A bounded on-device wait of an earlier product ran out: its outputs are void."""
+
+
+# The word that products report to when their caller gives none: pinned host memory, which the device writes
+# and the host reads without a synchronisation.
+_status_memory: Optional[torch.Tensor] = None
+_status_word = _i32(0)
+
+
+def _default_status() -> int:
+    """Its address; 0 if it would have to be allocated inside a stream capture."""
+    global _status_memory, _status_word
+    if _status_memory is None:
+        if torch.cuda.is_current_stream_capturing():
+            return 0
+        _status_memory = torch.zeros(1, dtype=torch.int32, pin_memory=True)
+        _status_word = _i32.from_address(_status_memory.data_ptr())
+    return _status_memory.data_ptr()
+
+
+def check_status() -> None:
+    """Raises ``WaitExpired`` if a product that was given no ``status`` ran out of a wait and has reported it by now.  Does not
+    synchronise: after a synchronisation it answers for everything before.  Every ``linear`` and ``linear_backward`` call
+    begins with this check."""
+    if _status_word.value:
+        _status_word.value = 0
+        raise WaitExpired("a bounded wait of an earlier linear or linear_backward call ran out; its outputs are void")
+
+
+def _status(status: Optional[torch.Tensor], dev: int) -> int:
+    """Pointer of the word that a call reports to."""
+    check_status()
+    return _default_status() if status is None else _full(status, (1,), torch.int32, dev, "status")
 
 
 def _stream(x: torch.Tensor) -> int:
@@ -314,12 +350,13 @@ def linear(x, weight, bias=None, activation: str = "none", residual=None, save_p
     """``themis_linear_forward``: ``act(x @ weight.T + bias) + residual``.
 
     ``x``: [rows, in]; ``weight``: [out, in]; ``bias``: float32 [out]; ``residual``: [rows, out].  With ``save_pre`` returns
-    ``(y, pre)``, ``pre`` being what ``linear_backward`` needs of an activation.  ``status``: int32 [1], see the header."""
+    ``(y, pre)``, ``pre`` being what ``linear_backward`` needs of an activation.  ``status``: int32 [1], see the header; without
+    it a wait that runs out is raised by a later call (``check_status``)."""
     dtype, dev, m, n, k, act = _linear_dims(x, weight, activation)
     (px, sx), (pw, sw) = _rows(x, m, k, dtype, dev, "x"), _rows(weight, n, k, dtype, dev, "weight")
     pr, sr = (None, n) if residual is None else _rows(residual, m, n, dtype, dev, "residual")
     pb = _full(bias, (n,), torch.float32, dev, "bias")
-    stream = _stream(x)
+    stream, word = _stream(x), _status(status, dev)
     problem = _LINEAR.pack(m, n, k, DTYPES[dtype], act, 0, sx, sw, sr, n)
     y = x.new_empty((m, n))
     pre = x.new_empty((m, n)) if save_pre else None
@@ -328,21 +365,21 @@ def linear(x, weight, bias=None, activation: str = "none", residual=None, save_p
     need = themis_linear_workspace_bytes(problem, False, unaligned) if unaligned or (sx | sw) & 7 else 0
     keep, ws, size = _workspace(need, workspace, x)
     _check(_lib.themis_linear_forward(problem, px, pw, pb, pr, y.data_ptr(), pre.data_ptr() if save_pre else None,
-                                      _full(status, (1,), torch.int32, dev, "status"), ws, size, stream), "themis_linear_forward")
+                                      word, ws, size, stream), "themis_linear_forward")
     return (y, pre) if save_pre else y
 
 
 def linear_backward(dy, x, weight, pre=None, activation: str = "none", bias: bool = True, need_dx: bool = True,
                     need_dweight: bool = True, status=None, workspace=None) -> dict:
     """``themis_linear_backward``: "dx" and "dweight" (the type of x), "dbias" (float32) as a dict.  The residual's gradient
-    is ``dy``."""
+    is ``dy``.  ``status``: as for ``linear``."""
     dtype, dev, m, n, k, act = _linear_dims(x, weight, activation)
     (px, sx), (pw, sw) = _rows(x, m, k, dtype, dev, "x"), _rows(weight, n, k, dtype, dev, "weight")
     pd, sd = _rows(dy, m, n, dtype, dev, "dy")
     if act and pre is None:
         raise TypeError("pre: an activation's gradient needs it")
     pp = _full(pre, (m, n), dtype, dev, "pre") if act else None
-    stream = _stream(x)
+    stream, word = _stream(x), _status(status, dev)
     problem = _LINEAR.pack(m, n, k, DTYPES[dtype], act, 0, sx, sw, n, sd)
     grads = {}
     if need_dx:
@@ -354,7 +391,7 @@ def linear_backward(dy, x, weight, pre=None, activation: str = "none", bias: boo
     keep, ws, size = _workspace(themis_linear_workspace_bytes(problem, True, bool((pd | px | pw) & 15)), workspace, x)
     _check(_lib.themis_linear_backward(
         problem, pd, px, pw, pp, *(grads[g].data_ptr() if g in grads else None for g in ("dx", "dweight", "dbias")),
-        _full(status, (1,), torch.int32, dev, "status"), ws, size, stream), "themis_linear_backward")
+        word, ws, size, stream), "themis_linear_backward")
     return grads
 
 

@@ -178,6 +178,7 @@ def main(argv=None) -> None:
     for t in range(args.seconds, args.seconds + args.ticks):
         predicted = model.tick(states, traces[:, t], t)
         stable += int(monitor(traces[:, t], predicted).sum())
+    forecast.check_status()
     print(f"{args.ticks} ticks of {args.pipelines} pipelines: {stable / (args.ticks * args.pipelines):.3f} of the workloads stable")
 
 

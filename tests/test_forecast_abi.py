@@ -165,3 +165,21 @@ def test_calls_on_cpu_tensors_are_refused(F):
     d = torch.zeros(2, 3, 8)
     with pytest.raises((TypeError, ValueError)):
         F.ssm_scan(d, d, torch.zeros(8, 4), torch.zeros(2, 3, 4), torch.zeros(2, 3, 4), torch.zeros(8, 4))
+
+
+def test_an_expired_wait_is_raised_by_the_next_call(F, monkeypatch):
+    """The host's side, with the device's write made by the test."""
+    import torch
+    F.check_status()
+    monkeypatch.setattr(F, "_status_word", ctypes.c_int32(F.STATUS_TIMEOUT))
+    with pytest.raises(F.WaitExpired):
+        F.check_status()
+    F.check_status()                                                         # raised once
+    word = torch.zeros(1, dtype=torch.int32)
+    monkeypatch.setattr(F, "_status_memory", word)
+    monkeypatch.setattr(F, "_status_word", ctypes.c_int32.from_address(word.data_ptr()))
+    assert F._status(None, 0) == word.data_ptr()
+    word[0] = F.STATUS_TIMEOUT
+    with pytest.raises(F.WaitExpired):
+        F._status(None, 0)
+    assert word.item() == 0

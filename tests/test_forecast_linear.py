@@ -272,3 +272,46 @@ def test_refusals(F):
     with pytest.raises(F.ThemisError) as e:
         F.linear_backward(a["residual"], a["x"], a["weight"], workspace=torch.empty(256, dtype=torch.uint8, device="cuda")[:0])
     assert e.value.code in (F.E_WORKSPACE_TOO_SMALL, F.E_INVALID_ARG)
+
+
+def test_an_expired_wait_is_not_lost(F, monkeypatch):
+    """Calls without a status, the autograd function's among them, report to one word of pinned host memory; what the
+    device writes there (here by a copy) is raised by the next call."""
+    a = make(100, 64, 48, torch.bfloat16)
+    y = F.linear(**a, activation="silu")
+    word = F._status_memory
+    assert word.is_pinned() and word.item() == 0
+    given = []
+    for name, at in (("themis_linear_forward", 7), ("themis_linear_backward", 8)):
+        real = getattr(F._lib, name)
+        monkeypatch.setattr(F._lib, name, lambda *args, real=real, at=at: (given.append(args[at]), real(*args))[1])
+    x = a["x"].clone().requires_grad_()
+    out = F.Linear.apply(x, a["weight"], a["bias"], "silu", a["residual"])
+    out.sum().backward()
+    assert given == [word.data_ptr()] * 2 and torch.equal(out, y)
+    torch.cuda.synchronize()
+    F.check_status()
+    expired = torch.full((1,), F.STATUS_TIMEOUT, dtype=torch.int32, device="cuda")
+    for call in (lambda: F.linear(**a), lambda: F.linear_backward(a["residual"], a["x"], a["weight"]),
+                 lambda: F.Linear.apply(x, a["weight"]), F.check_status):
+        word.copy_(expired)
+        with pytest.raises(F.WaitExpired):
+            call()
+        assert torch.equal(F.linear(**a, activation="silu"), y)
+    # a word of the caller's own is used as it is
+    own = torch.zeros(1, dtype=torch.int32, device="cuda")
+    F.linear(**a, status=own)
+    assert given[-1] == own.data_ptr() and own.item() == 0
+
+
+def test_capture_into_a_graph(F):
+    a = make(100, 64, 48, torch.bfloat16)
+    y = F.linear(**a, activation="silu")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        again = F.linear(**a, activation="silu")
+    again.zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(again, y)
+    F.check_status()
