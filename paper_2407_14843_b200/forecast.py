@@ -295,8 +295,30 @@ def ssm_step(x, dt, A, B, C, conv_weight, conv_bias=None, skip=None, dt_bias=Non
     return y
 
 
+class _FirstOrderOnly(torch.autograd.Function):
+    """A gradient as it is; differentiating it raises."""
+
+    @staticmethod
+    def forward(ctx, anchor, grad):
+        return grad.view_as(grad)
+
+    @staticmethod
+    def backward(ctx, _):
+        raise RuntimeError("the gradients of SsmScan and Linear cannot be differentiated again")
+
+
+def _first_order(grads):
+    """Gradients made by kernels, which autograd cannot see into: with ``create_graph=True`` they depend on a node that
+    raises, so that a second derivative is refused instead of being taken as 0."""
+    if not torch.is_grad_enabled():
+        return grads
+    anchor = torch.empty(0, requires_grad=True)
+    return tuple(None if g is None else _FirstOrderOnly.apply(anchor, g) for g in grads)
+
+
 class SsmScan(torch.autograd.Function):
-    """``SsmScan.apply(x, dt, A, B, C, conv_weight, conv_bias, skip, dt_bias, z, lengths)`` -> y, from zero states."""
+    """``SsmScan.apply(x, dt, A, B, C, conv_weight, conv_bias, skip, dt_bias, z, lengths)`` -> y, from zero states.  Has first
+    derivatives only."""
 
     @staticmethod
     def forward(ctx, x, dt, A, B, C, conv_weight, conv_bias=None, skip=None, dt_bias=None, z=None, lengths=None):
@@ -309,7 +331,8 @@ class SsmScan(torch.autograd.Function):
     def backward(ctx, dy):
         checkpoints, lengths, *args = ctx.saved_tensors
         g = ssm_scan_backward(dy.contiguous(), checkpoints, *args, lengths=lengths)
-        return tuple(g.get(k) for k in ("dx", "ddt", "dA", "dB", "dC", "dconv_weight", "dconv_bias", "dskip", "ddt_bias", "dz")) + (None,)
+        names = ("dx", "ddt", "dA", "dB", "dC", "dconv_weight", "dconv_bias", "dskip", "ddt_bias", "dz")
+        return _first_order(tuple(g.get(k) for k in names)) + (None,)
 
 
 # --- linear ----------------------------------------------------------------------------------------
@@ -396,7 +419,7 @@ def linear_backward(dy, x, weight, pre=None, activation: str = "none", bias: boo
 
 
 class Linear(torch.autograd.Function):
-    """``Linear.apply(x, weight, bias, activation, residual)`` -> y."""
+    """``Linear.apply(x, weight, bias, activation, residual)`` -> y.  Has first derivatives only."""
 
     @staticmethod
     def forward(ctx, x, weight, bias=None, activation="none", residual=None):
@@ -409,8 +432,9 @@ class Linear(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dy):
         x, weight, pre = ctx.saved_tensors
+        residual = dy if ctx.has_residual else None
         if dy.stride(-1) != 1 or (dy.shape[0] > 1 and dy.stride(0) < dy.shape[1]):
             dy = dy.contiguous()
         need = ctx.needs_input_grad
         g = linear_backward(dy, x, weight, pre, ctx.activation, bias=ctx.has_bias and need[2], need_dx=need[0], need_dweight=need[1])
-        return g.get("dx"), g.get("dweight"), g.get("dbias"), None, dy if ctx.has_residual else None
+        return _first_order((g.get("dx"), g.get("dweight"), g.get("dbias"))) + (None, residual)

@@ -315,3 +315,19 @@ def test_capture_into_a_graph(F):
     torch.cuda.synchronize()
     assert torch.equal(again, y)
     F.check_status()
+
+
+@pytest.mark.parametrize("activation", ["none", "silu"])
+def test_second_derivatives_are_refused(F, activation):
+    """Alone and in a sum with other terms, where a gradient without a graph would only go missing."""
+    a = make(50, 40, 24, torch.bfloat16, seed=3)
+    for name in ("x", "weight", "bias"):
+        leaves = {k: v.clone().requires_grad_() for k, v in a.items()}
+        y = F.Linear.apply(leaves["x"], leaves["weight"], leaves["bias"], activation, leaves["residual"])
+        g, = torch.autograd.grad(y.float().square().sum() if name == "x" else y.sum(), leaves[name], create_graph=True)
+        plain = {k: v.clone().requires_grad_() for k, v in a.items()}
+        y = F.Linear.apply(plain["x"], plain["weight"], plain["bias"], activation, plain["residual"])
+        want, = torch.autograd.grad(y.float().square().sum() if name == "x" else y.sum(), plain[name])
+        assert torch.equal(g, want) and g.requires_grad
+        with pytest.raises(RuntimeError, match="differentiated again"):
+            (g.float().square().sum() + leaves["x"].float().sum()).backward()

@@ -424,3 +424,17 @@ def test_parts_of_several_tiles(F, state, views, dtype):
     s = F.ssm_scan(**spoil(ragged), states=False)
     for b, n in enumerate(ragged["lengths"].tolist()):
         assert torch.equal(s.y[b, :n], r.y[b, :n]) and (s.y[b, n:] == 0).all()
+
+
+@pytest.mark.parametrize("name", ["x", "dt", "A", "B", "C", "conv_weight", "conv_bias", "skip", "dt_bias", "z"])
+def test_second_derivatives_are_refused(F, name):
+    """Alone and in a sum with other terms, where a gradient without a graph would only go missing."""
+    a = make(3, 20, 24, 8, states=False, views=False, seed=12)
+    names = ("x", "dt", "A", "B", "C", "conv_weight", "conv_bias", "skip", "dt_bias", "z")
+    leaves = [a[k].clone().requires_grad_() for k in names]
+    at = leaves[names.index(name)]
+    want, = torch.autograd.grad(F.SsmScan.apply(*leaves, None).sum(), at)
+    g, = torch.autograd.grad(F.SsmScan.apply(*leaves, None).sum(), at, create_graph=True)
+    assert torch.equal(g, want) and g.requires_grad
+    with pytest.raises(RuntimeError, match="differentiated again"):
+        (g.square().sum() + at.sum()).backward()
