@@ -3,6 +3,7 @@
 
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
+#include <float.h>
 #include <stdint.h>
 
 namespace themis {
@@ -155,6 +156,13 @@ __device__ __forceinline__ f32x2 ex2_pair(f32x2 v)
 // is raised by kExpShift in the multiply-add that forms it: -0.7e-8 to +0.4e-8 on average for exponents
 // of 0.0002 to 0.02 and within 1.5e-8 up to 1.  exp(0) stays 1.
 constexpr float kExpShift = 1.3e-8f;
+// A log2(e), kept finite (NaN stays): a time that does not exist has a step of 0 and its factor has to be 1 for
+// the lowest A and for -inf too, where 0 times an infinity would be no number.
+__device__ __forceinline__ float log2_rate(float a)
+{
+    const float v = a * kLog2e;
+    return v < -FLT_MAX ? -FLT_MAX : v > FLT_MAX ? FLT_MAX : v;
+}
 __device__ __forceinline__ float decay(float s, float a2) { return ex2(fmaf(s, a2, kExpShift)); }
 __device__ __forceinline__ f32x2 decay2(f32x2 s, f32x2 a2) { return ex2_pair(fma2(s, a2, pack2(kExpShift, kExpShift))); }
 

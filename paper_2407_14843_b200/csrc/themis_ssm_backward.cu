@@ -191,7 +191,7 @@ __global__ __launch_bounds__(128, sizeof(T) == 4 ? 3 : 4) void ssm_adjoint_local
 #pragma unroll
     for (int i = 0; i < NPT / 2; ++i) {
         const int n = n0 + 2 * i;
-        a2[i] = pack2(n < N ? p.in.a[(size_t)dr * N + n] * kLog2e : 0.0f, n + 1 < N ? p.in.a[(size_t)dr * N + n + 1] * kLog2e : 0.0f);
+        a2[i] = pack2(n < N ? log2_rate(p.in.a[(size_t)dr * N + n]) : 0.0f, n + 1 < N ? log2_rate(p.in.a[(size_t)dr * N + n + 1]) : 0.0f);
         acc[i] = pack2(0.0f, 0.0f);
     }
     float sum = 0.0f;
@@ -273,7 +273,7 @@ __global__ void ssm_adjoint_join_kernel(const SsmParams p)
     const int e = blockIdx.y * blockDim.x + threadIdx.x, b = blockIdx.x;
     if (e >= DN) return;
     const int d = e / N;
-    const float a = p.in.a[e] * kLog2e;
+    const float a = log2_rate(p.in.a[e]);
     float *st = p.split_state + (size_t)b * p.splits * DN + e;
     const float *sum = p.split_step + (size_t)b * p.splits * D + d;
     float q = 0.0f;
@@ -356,7 +356,7 @@ __global__ __launch_bounds__(Shape<T, LPC>::THREADS, Shape<T, LPC>::RESIDENT) vo
         for (int j = 0; j < 2; ++j) {
             const bool in = n0 + i < N && c0 + j < nd;
             const size_t at = (size_t)(d0 + c0 + j) * N + n0 + i;
-            av[j] = in ? p.in.a[at] * kLog2e : 0.0f;
+            av[j] = in ? log2_rate(p.in.a[at]) : 0.0f;
             qv[j] = in && p.splits > 1 ? p.split_state[((size_t)b * p.splits + split) * D * N + at] : 0.0f;
         }
         A2[i] = pack2(av[0], av[1]);

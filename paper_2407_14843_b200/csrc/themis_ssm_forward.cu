@@ -109,7 +109,7 @@ __global__ __launch_bounds__(kThreads, kPlaces<T>) void ssm_scan_kernel(const Ss
             for (int j = 0; j < 2; ++j) {
                 const int n = 2 * i + j;
                 const bool in = n0 + n < N;
-                a[j] = in ? p.in.a[(size_t)dr * N + n0 + n] * kLog2e : 0.0f;
+                a[j] = in ? log2_rate(p.in.a[(size_t)dr * N + n0 + n]) : 0.0f;
                 was[j] = in && hs ? hs[n] : 0.0f;
             }
             a2[i] = pack2(a[0], a[1]);
@@ -321,7 +321,7 @@ __global__ void ssm_join_kernel(const SsmParams p)
     const int e = blockIdx.y * blockDim.x + threadIdx.x, b = blockIdx.x;
     if (e >= DN) return;
     const int d = e / N;
-    const float a = p.in.a[e] * kLog2e;
+    const float a = log2_rate(p.in.a[e]);
     float h = p.in.ssm_state ? p.in.ssm_state[(size_t)b * DN + e] : 0.0f;
     float *st = p.split_state + (size_t)b * p.splits * DN + e;
     const float *sum = p.split_step + (size_t)b * p.splits * D + d;

@@ -68,7 +68,7 @@ __device__ __forceinline__ void step_rows(const SsmParams &p, int l, int64_t b0)
     float A[4];
     load4<float, VEC>(p.in.a + (size_t)dd * N + n0, nn, A);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) A[i] *= kLog2e;
+    for (int i = 0; i < 4; ++i) A[i] = log2_rate(A[i]);
 
     Pair<T> bq[ROWS][2], cq[ROWS][2];       // B and C of the rows, as they are
     if (VEC) {

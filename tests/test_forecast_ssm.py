@@ -438,3 +438,28 @@ def test_second_derivatives_are_refused(F, name):
     assert torch.equal(g, want) and g.requires_grad
     with pytest.raises(RuntimeError, match="differentiated again"):
         (g.square().sum() + at.sum()).backward()
+
+
+@pytest.mark.parametrize("length", [1, 6, 61, 700])
+def test_states_that_forget_at_once(F, length):
+    """A of the lowest value and of -inf: the factors are 0 at every time that exists and 1 at those that do not
+    (behind a row's end, and up to the next multiple of the times that a kernel takes at once)."""
+    rows = 3
+    a = make(rows, length, 24, 8, dtype=torch.bfloat16, seed=40 + length, views=False)
+    a["A"][:, 1], a["A"][:, 5], a["A"][3] = torch.finfo(torch.float32).min, -math.inf, -math.inf
+    for lengths in (None, torch.tensor([0, max(1, length // 3), length], dtype=torch.int32, device="cuda")):
+        b = dict(a) if lengths is None else dict(a, lengths=lengths)
+        r = F.ssm_scan(**(b if lengths is None else spoil(b)))
+        y, conv, h = R.scan(**b)
+        R.close(r.y, y, terms=512, what="y")
+        R.close(r.ssm_state, h, terms=512, what="state")
+        assert torch.equal(r.conv_state.double(), conv)
+    s = {k: (v[:, 0] if k in ("x", "dt", "z", "B", "C") else v.clone()) for k, v in a.items()}
+    y, _, h = R.scan(**{k: (v[:, :1] if k in ("x", "dt", "z", "B", "C") else v) for k, v in a.items()})
+    R.close(F.ssm_step(**s), y[:, 0], what="y of a step")
+    R.close(s["ssm_state"], h, what="state of a step")
+    # gradients for finite A (those of -inf are not a number by the formula: A exp(s A))
+    a["A"] = a["A"].clamp_min(torch.finfo(torch.float32).min)
+    lengths = torch.tensor([0, max(1, length // 3), length], dtype=torch.int32, device="cuda")
+    dy = torch.randn(rows, length, 24, device="cuda").bfloat16()
+    check_gradients(F, dict(a, lengths=lengths), dy, terms=1024, spoiled=spoil(dict(a, lengths=lengths)))
