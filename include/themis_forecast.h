@@ -55,8 +55,8 @@ extern "C" {
 
 typedef struct {
     int32_t batch;      /* rows, >= 0 */
-    int32_t length;     /* times, >= 0 (step: ignored, one) */
-    int32_t channels;   /* D >= 1 */
+    int32_t length;     /* times, in 0..2^30 (step: not used, one) */
+    int32_t channels;   /* D in 1..65535 */
     int32_t state;      /* N in 1..THEMIS_SSM_MAX_STATE */
     int32_t groups;     /* G >= 1, divides channels: channel d uses group d / (D / G) */
     int32_t conv_width; /* W in 2..4 */

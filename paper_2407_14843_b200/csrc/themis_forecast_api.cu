@@ -15,7 +15,7 @@ inline size_t size_of(int32_t dtype) { return dtype == THEMIS_DTYPE_F32 ? 4 : 2;
 
 // --- selective scan ---------------------------------------------------------------------------
 
-int validate_ssm(const themis_ssm_problem_t *pr)
+int validate_ssm(const themis_ssm_problem_t *pr, bool step = false)
 {
     if (!pr) return THEMIS_E_INVALID_ARG;
     if (pr->batch < 0 || pr->length < 0 || pr->channels < 1 || pr->state < 1 || pr->groups < 1) return THEMIS_E_INVALID_ARG;
@@ -27,6 +27,7 @@ int validate_ssm(const themis_ssm_problem_t *pr)
         if (s < 0) return THEMIS_E_INVALID_ARG;
     if (pr->state > THEMIS_SSM_MAX_STATE) return THEMIS_E_UNSUPPORTED_SIZE;
     if (pr->conv_width < THEMIS_SSM_MIN_CONV || pr->conv_width > THEMIS_SSM_MAX_CONV) return THEMIS_E_UNSUPPORTED_SIZE;
+    if (!step && pr->length > (1 << 30)) return THEMIS_E_UNSUPPORTED_SIZE;    // times are 32-bit, up to the end of the last part
     if (pr->channels > 65535) return THEMIS_E_UNSUPPORTED_SIZE;      // tiles of channels are a grid's second axis
     return THEMIS_OK;
 }
@@ -189,7 +190,7 @@ int themis_ssm_backward(const themis_ssm_problem_t *problem, const themis_ssm_in
 int themis_ssm_step(const themis_ssm_problem_t *problem, const themis_ssm_inputs_t *in,
                     const themis_ssm_outputs_t *out, void *cuda_stream)
 {
-    int rc = validate_ssm(problem);
+    int rc = validate_ssm(problem, true);
     if (rc != THEMIS_OK) return rc;
     if (!in || !out) return THEMIS_E_INVALID_ARG;
     if (problem->batch == 0) return THEMIS_OK;

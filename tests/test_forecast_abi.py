@@ -183,3 +183,17 @@ def test_an_expired_wait_is_raised_by_the_next_call(F, monkeypatch):
     with pytest.raises(F.WaitExpired):
         F._status(None, 0)
     assert word.item() == 0
+
+
+def test_lengths_that_leave_no_room_to_round_up_are_refused(F):
+    """Times are counted in 32 bits, up to the next multiple of a part."""
+    n, count = ctypes.c_size_t(), ctypes.c_int32()
+    for length, code in ((2 ** 30, F.OK), (2 ** 30 + 1, F.E_UNSUPPORTED_SIZE), (2 ** 31 - 1, F.E_UNSUPPORTED_SIZE)):
+        p = bytes(ssm(F, batch=1, length=length, channels=1, state=1))
+        assert F._lib.themis_ssm_checkpoints(p, ctypes.byref(count)) == code
+        assert F._lib.themis_ssm_workspace_bytes(p, 0, ctypes.byref(n)) == code
+        assert F._lib.themis_ssm_workspace_bytes(p, 1, ctypes.byref(n)) == code
+        if code == F.OK:
+            assert count.value == length // F.SSM_CHUNK
+    # a step has no use for it
+    assert F._lib.themis_ssm_step(bytes(ssm(F, batch=0, length=2 ** 31 - 1)), F._INPUTS.pack(*[0] * 13), F._OUTPUTS.pack(*[0] * 4), None) == F.OK
