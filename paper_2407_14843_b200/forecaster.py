@@ -23,6 +23,7 @@ from . import forecast
 
 HORIZON = 10        # seconds ahead whose largest rate is predicted
 N_FEATURES = 8      # inputs of a second (three used; rows of 16 bytes)
+MIN_RATE = 1e-3     # rps; what an idle second counts as, in features, targets and predictions alike
 
 
 def features(rates: torch.Tensor, first_second: int = 0) -> torch.Tensor:
@@ -30,7 +31,7 @@ def features(rates: torch.Tensor, first_second: int = 0) -> torch.Tensor:
     t = torch.arange(first_second, first_second + rates.shape[1], device=rates.device, dtype=torch.float32)
     phase = (2 * math.pi / 86400) * t
     out = torch.zeros(*rates.shape, N_FEATURES, device=rates.device)
-    out[..., 0] = 0.25 * torch.log(rates.float().clamp(min=1e-3))
+    out[..., 0] = 0.25 * torch.log(rates.float().clamp(min=MIN_RATE))
     out[..., 1] = torch.sin(phase)
     out[..., 2] = torch.cos(phase)
     return out.bfloat16()
@@ -100,7 +101,7 @@ class RateForecaster:
         """Mean squared error of the predicted logarithm over [batch, length + HORIZON] rates."""
         seen = rates[:, :-HORIZON]
         ahead = rates[:, 1:].unfold(1, HORIZON, 1).amax(-1)
-        target = torch.log(ahead.clamp(min=1e-3) / seen.clamp(min=1e-3))
+        target = torch.log(ahead.clamp(min=MIN_RATE) / seen.clamp(min=MIN_RATE))
         out, _ = self._scan(features(seen), None, False)
         return (out - target.flatten()).square().mean()
 
@@ -125,7 +126,7 @@ class RateForecaster:
             a, conv, conv_bias, skip, dt_bias = self._parameters(i)
             y = forecast.ssm_step(u, dt, a, b, c, conv, conv_bias, skip, dt_bias, z, conv_state=conv_state, ssm_state=ssm_state)
             h = forecast.linear(y, self._w(f"out{i}"), self.params[f"out_bias{i}"], residual=h)
-        return rates.float() * torch.exp(self._head(h))
+        return rates.float().clamp(min=MIN_RATE) * torch.exp(self._head(h))
 
 
 def to_mrps(rates: torch.Tensor) -> torch.Tensor:
