@@ -57,7 +57,6 @@ template <typename T, int LPC> struct Shape {
     static constexpr int PARTS = (!IN_SLOT ? kSubs : SHARE ? 1 : 2) * WARPS * PART;
     // u, s, e; states before sub-chunks 1 .. kSubs - 2; B and C; partial sums; carry; parameters; dA
     static constexpr int FLOATS = 3 * kChunk * CT + (kSubs - 2) * SLOT + kChunk * 2 * NP + PARTS + (3 + kPars) * CT + SLOT;
-    static constexpr int RESIDENT = LPC == 4 || LPC == 8 ? 2 : 3;   // blocks of a multiprocessor
     // The inputs of a chunk as they are; 16-bit ones twice, the next chunk's arriving meanwhile (two
     // buffers of 32-bit ones would leave room for one block to a multiprocessor).
     struct Raw {                                                 // (every array on the 16 bytes of a copy)
@@ -70,6 +69,10 @@ template <typename T, int LPC> struct Shape {
     };
     static constexpr int BUFS = sizeof(T) == 4 ? 1 : 2;
     static constexpr size_t BYTES = FLOATS * sizeof(float) + BUFS * sizeof(Raw);
+    // Blocks of a multiprocessor: by registers (128 a thread in blocks of 256, 168 in blocks of 128) and by
+    // the shared memory that each takes with its reserved kilobyte, which leaves two for up to 8 states.  (A
+    // training step 16 x 2048 x 1024 with 4 states, bf16: 1348 us compiled and planned for three, 1276 for two.)
+    static constexpr int RESIDENT = std::min<int>(WARPS == 8 ? 2 : 3, 228 * 1024 / (BYTES + 1024));
 };
 
 // First pass over split parts: NPT states to a lane, LPC lanes to a channel, as in the forward kernel.
@@ -313,6 +316,7 @@ __global__ __launch_bounds__(Shape<T, LPC>::THREADS, Shape<T, LPC>::RESIDENT) vo
     float(*s_carry)[CT] = reinterpret_cast<float(*)[CT]>(take(3 * CT));         // dc of the next chunk's first times
     float(*s_par)[CT] = reinterpret_cast<float(*)[CT]>(take(kPars * CT));
     using Raw = typename S::Raw;
+    static_assert(S::RESIDENT == Shape<float, LPC>::RESIDENT && S::CT == Shape<float, LPC>::CT, "the plan takes both from the 32-bit shape");
     static_assert(sizeof(Raw) % 16 == 0 && offsetof(Raw, x) % 16 == 0 && offsetof(Raw, dt) % 16 == 0 && offsetof(Raw, z) % 16 == 0 &&
                       offsetof(Raw, dy) % 16 == 0 && offsetof(Raw, b) % 16 == 0 && offsetof(Raw, c) % 16 == 0,
                   "rows are copied and read 16 bytes at a time");
@@ -836,8 +840,12 @@ template <typename T> cudaError_t launch_shape(const SsmParams &p, cudaStream_t 
 
 void ssm_backward_plan(const themis_ssm_problem_t *pr, SsmParams *p)
 {
+    // (the two are the same for every type: two 16-bit input buffers are as large as one of 32 bits)
     const int ct = pr->state <= 8 ? Shape<float, 2>::CT : pr->state <= 16 ? Shape<float, 4>::CT : pr->state <= 32 ? Shape<float, 8>::CT : Shape<float, 16>::CT;
-    const int resident = pr->state <= 8 ? Shape<float, 2>::RESIDENT : pr->state <= 32 ? Shape<float, 4>::RESIDENT : Shape<float, 16>::RESIDENT;
+    const int resident = pr->state <= 8    ? Shape<float, 2>::RESIDENT
+                         : pr->state <= 16 ? Shape<float, 4>::RESIDENT
+                         : pr->state <= 32 ? Shape<float, 8>::RESIDENT
+                                           : Shape<float, 16>::RESIDENT;
     p->tiles_per_group = (pr->channels / pr->groups + ct - 1) / ct;
     p->n_chunks = (pr->length + kChunk - 1) / kChunk;
     const long long blocks = (long long)p->tiles_per_group * pr->groups * pr->batch;
