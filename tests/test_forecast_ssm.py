@@ -463,3 +463,82 @@ def test_states_that_forget_at_once(F, length):
     lengths = torch.tensor([0, max(1, length // 3), length], dtype=torch.int32, device="cuda")
     dy = torch.randn(rows, length, 24, device="cuda").bfloat16()
     check_gradients(F, dict(a, lengths=lengths), dy, terms=1024, spoiled=spoil(dict(a, lengths=lengths)))
+
+
+# --- fleets: what many rows run -------------------------------------------------------------------
+
+DTYPES = pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16], ids=["fp32", "bf16", "fp16"])
+
+
+@DTYPES
+@pytest.mark.parametrize("views", [False, True], ids=["aligned", "unaligned"])
+@pytest.mark.parametrize("shape", [(2371, 264, 16, 1, 4), (2371, 263, 16, 1, 4), (2370, 264, 12, 1, 4), (4603, 264, 8, 2, 3), (1151, 264, 32, 1, 4),
+                                   (579, 264, 64, 1, 2), (9301, 264, 4, 3, 4)], ids=str)
+def test_step_of_many_rows(F, shape, views, dtype):
+    """Several rows to a thread (two times 1.2 million lanes and more): whole blocks, the last block of a row, a rest of
+    rows, inactive rows with NaN, states in place and elsewhere."""
+    rows, D, N, G, W = shape
+    a = make(rows, 1, D, N, G, W, dtype=dtype, seed=N, views=views)
+    y, conv, h = R.scan(**a)
+    s = {k: (v[:, 0] if k in ("x", "dt", "z", "B", "C") else v) for k, v in a.items()}
+    kept = a["conv_state"].clone(), a["ssm_state"].clone()
+    new_conv, new_h = torch.full_like(kept[0], 7), torch.full_like(kept[1], 7)
+    got = F.ssm_step(**s, new_conv_state=new_conv, new_ssm_state=new_h)
+    R.close(got, y[:, 0], what="y")
+    R.close(new_h, h, what="state")
+    assert torch.equal(new_conv.double(), conv)
+    assert torch.equal(a["conv_state"], kept[0]) and torch.equal(a["ssm_state"], kept[1])
+    active = (torch.arange(rows, device="cuda") * 2654435761 % 7 < 5).int()
+    active[-1] = 0
+    off = active == 0
+    for k in ("x", "dt", "z", "B", "C"):
+        s[k][off] = float("nan")
+    in_place = F.ssm_step(**s, active=active)
+    assert (in_place[off] == 0).all() and torch.equal(in_place[~off], got[~off])
+    assert torch.equal(a["ssm_state"][~off], new_h[~off]) and torch.equal(a["conv_state"][~off], new_conv[~off])
+    assert torch.equal(a["ssm_state"][off], kept[1][off]) and torch.equal(a["conv_state"][off], kept[0][off])
+
+
+def check_all(F, a, dy, terms):
+    """Forward and gradients against 64 bits."""
+    leaves = {k: a[k].detach().double().requires_grad_() for k in NAMES if k in a}
+    y, conv, h = R.scan(**{**a, **leaves})
+    ref = dict(zip((NAMES[k] for k in leaves), torch.autograd.grad(y, list(leaves.values()), dy.double())))
+    given = spoil(a) if "lengths" in a else a
+    plain = F.ssm_scan(**given)
+    r = F.ssm_scan(**given, save=True)
+    assert torch.equal(plain.y, r.y) and torch.equal(plain.ssm_state, r.ssm_state)
+    R.close(r.y, y.detach(), what="y")
+    R.close(r.ssm_state, h.detach(), what="state")
+    assert torch.equal(r.conv_state.double(), conv.detach())
+    got = F.ssm_scan_backward(dy, r.checkpoints, **given)
+    assert set(got) == set(ref)
+    for k in ref:
+        R.close(got[k], ref[k], terms=terms, what=k)
+
+
+# rows, length, D, N, G, W; enough rows for 16 states on a lane (with 1, 2 and 4 lanes to a channel) and 8 (1, 2)
+FLEETS = [(90, 37, 504, 16, 1, 4), (90, 37, 505, 13, 1, 3), (124, 40, 264, 8, 1, 4), (204, 35, 136, 5, 1, 2), (124, 40, 136, 16, 1, 4),
+          (124, 33, 272, 24, 2, 4), (30, 70, 136, 64, 1, 4)]
+
+
+@DTYPES
+@pytest.mark.parametrize("ragged", [False, True], ids=["whole", "ragged"])
+@pytest.mark.parametrize("shape", FLEETS, ids=str)
+def test_many_rows(F, shape, ragged, dtype):
+    a = make(*shape, dtype=dtype, seed=sum(shape), ragged=ragged, views=ragged)
+    dy = torch.randn(shape[0], shape[1], shape[2], device="cuda").to(dtype)
+    # parameters' gradients sum rows x times (about 4000) terms of some tens of roundings each: 64 times the square root
+    check_all(F, a, dy, terms=1024)
+
+
+@DTYPES
+@pytest.mark.parametrize("views", [False, True], ids=["aligned", "unaligned"])
+@pytest.mark.parametrize("shape", [(300, 197, 40, 16, 1, 4), (300, 200, 40, 32, 1, 3), (450, 150, 24, 40, 1, 4), (600, 150, 40, 8, 1, 4),
+                                   (600, 150, 40, 4, 1, 4), (600, 131, 40, 3, 1, 2)], ids=str)
+def test_gradients_of_many_chunks_in_one_part(F, shape, views, dtype):
+    """Rows that fill the GPU are not split: nine to thirteen chunks one after the other in a block."""
+    a = make(*shape, dtype=dtype, seed=sum(shape), views=views)
+    assert parts_of(F, a, True) == 1
+    dy = torch.randn(shape[0], shape[1], shape[2], device="cuda").to(dtype)
+    check_all(F, a, dy, terms=1024)
