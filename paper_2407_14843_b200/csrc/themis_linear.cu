@@ -156,6 +156,10 @@ cudaError_t aligned_rows(const void *&ptr, int64_t &pitch, int rows, int width, 
 // Reads dy and pre once and writes q once.  A block takes 256 columns of some rows, 8 columns
 // to a thread (VEC) and 8 threads to a column; the sums of q over the block's rows are added in
 // shared memory and, over the blocks, by column_sum_kernel, always in the same order.
+// q is rounded to the 16 bits of the other operand, because a tensor-core product takes both in that type; its
+// low bits as a second product would double the time of both.  The relative error of dx and dweight against 64 bits
+// grows by it from 0.0017 to 0.0023 in bf16 (32768 x 4096 x 1024) and from 0.00021 to 0.00029 in fp16 (777 x 328 x
+// 200), of which the outputs' own rounding is the first number.  The bias gradient sums q unrounded, in 32 bits.
 // rows of a block: 64, or 16 where those would be too few blocks to fill the GPU (777 x 328 with gelu: 16 us
 // with 64, 5 us with 16)
 inline int slope_rows(int M, int N) { return (long long)((N + 255) / 256) * ((M + 63) / 64) >= 2 * kSMs ? 64 : 16; }

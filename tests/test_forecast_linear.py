@@ -331,3 +331,39 @@ def test_second_derivatives_are_refused(F, activation):
         assert torch.equal(g, want) and g.requires_grad
         with pytest.raises(RuntimeError, match="differentiated again"):
             (g.float().square().sum() + leaves["x"].float().sum()).backward()
+
+
+@TYPES
+@pytest.mark.parametrize("rows", [4, 200])
+@pytest.mark.parametrize("activation", ["silu", "gelu"])
+def test_activations_value_by_value(F, activation, rows, dtype):
+    """pre is the bias alone, over -12..12, and every value has its own room: one rounding to the type; for gelu
+    1.5e-7 / 2 of v (the error function's) and four roundings of the distribution function, from -6 to -3 also no more
+    than 4e-3 of the value; for silu a dozen roundings and the exponent's |v|."""
+    v = torch.linspace(-12, 12, 4097, device="cuda")[:4096].contiguous()
+    x = torch.ones(rows, 16, dtype=dtype, device="cuda")
+    y = F.linear(x, torch.zeros(4096, 16, dtype=dtype, device="cuda"), v, activation).double()
+    d = v.double()
+    # (1 + erf would cancel in 64 bits too)
+    ref = d * 0.5 * torch.special.erfc(-d / math.sqrt(2)) if activation == "gelu" else d / (1 + torch.exp(-d))
+    room = 1.01 * R.UNIT[dtype] * ref.abs() + (2.0 ** -25 if dtype == torch.float16 else 1e-36)
+    if activation == "gelu":
+        wide = d.abs() * (0.75e-7 + 4 * 2.0 ** -24)
+        tail = (d >= -6) & (d <= -3)
+        room = room + torch.where(tail, torch.minimum(wide, 4e-3 * ref.abs()), wide)
+    else:
+        room = room + ref.abs() * (12 + d.abs()) * 2.0 ** -24
+    assert ((y - ref).abs() <= room).all(), ((y - ref).abs() / room).max().item()
+
+
+@TYPES
+@pytest.mark.parametrize("activation", ["silu", "gelu"])
+def test_slopes_value_by_value(F, activation, dtype):
+    """The bias gradient of one row with dy = 1 is the slope in 32 bits: the error function's 0.75e-7 and sixteen
+    roundings of values up to 1.13."""
+    pre = torch.linspace(-12, 12, 4097, device="cuda")[:4096].to(dtype)[None]
+    x, w = torch.zeros(1, 16, dtype=dtype, device="cuda"), torch.zeros(4096, 16, dtype=dtype, device="cuda")
+    got = F.linear_backward(torch.ones_like(pre), x, w, pre=pre, activation=activation)["dbias"].double()
+    p = pre[0].double().requires_grad_()
+    ref, = torch.autograd.grad(R.activate(p, activation).sum(), p)
+    assert (got - ref).abs().max() <= 0.75e-7 + 16 * 1.13 * 2.0 ** -24
