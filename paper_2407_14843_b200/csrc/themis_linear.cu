@@ -119,7 +119,7 @@ __global__ __launch_bounds__(256) void copy_rows_kernel(const T *from, int64_t f
         uint32_t v[U];
 #pragma unroll
         for (int k = 0; k < U; ++k)
-            if (r0 + k < rows) v[k] = load_pair(from + (r0 + k) * from_row + c, false, two);
+            if (r0 + k < rows) v[k] = load_two(from + (r0 + k) * from_row + c, two);
 #pragma unroll
         for (int k = 0; k < U; ++k)
             if (r0 + k < rows) *reinterpret_cast<uint32_t *>(to + (r0 + k) * to_row + c) = v[k];

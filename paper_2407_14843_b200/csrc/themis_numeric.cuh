@@ -35,19 +35,11 @@ template <typename T> __device__ __forceinline__ bool pairs_ok(const T *first, i
 {
     return two && ((uintptr_t)first & (2 * sizeof(T) - 1)) == 0 && (stride & 1) == 0;
 }
-// `pair`: one access; otherwise two, or one value twice (!two)
-__device__ __forceinline__ uint2 load_pair(const float *p, bool pair, bool two)
+// two neighbouring 16-bit values, or one twice (!two)
+template <typename T> __device__ __forceinline__ uint32_t load_two(const T *p, bool two)
 {
-    if (pair) return *reinterpret_cast<const uint2 *>(p);
-    return make_uint2(__float_as_uint(p[0]), __float_as_uint(p[two ? 1 : 0]));
-}
-template <typename T> __device__ __forceinline__ uint32_t load_pair(const T *p, bool pair, bool two)
-{
-    if (pair) return *reinterpret_cast<const uint32_t *>(p);
     return bits_of(p[0]) | bits_of(p[two ? 1 : 0]) << 16;
 }
-__device__ __forceinline__ uint2 drop_second(uint2 v) { return make_uint2(v.x, 0); }
-__device__ __forceinline__ uint32_t drop_second(uint32_t v) { return v & 0xffffu; }
 
 template <typename T> struct Unpack;
 template <> struct Unpack<float> {

@@ -64,7 +64,7 @@ template <typename T, int PITCH, int ROWS, int THREADS> struct RowCopy {
                 if (off[k] != ~0u) async16(dst + (tid + k * THREADS) * V, base + off[k]);
             return;
         }
-if (vec && width % V == 0) {                  // the row's ends
+        if (vec && width % V == 0) {                     // the row's ends
 #pragma unroll 1
             for (int i = tid; i < ITEMS; i += THREADS) {
                 const int c = i % PER * V, t = t0 + i / PER;
