@@ -850,9 +850,10 @@ void ssm_backward_plan(const themis_ssm_problem_t *pr, SsmParams *p)
     p->n_chunks = (pr->length + kChunk - 1) / kChunk;
     const long long blocks = (long long)p->tiles_per_group * pr->groups * pr->batch;
     // Time of a part's chunk with k blocks on a multiprocessor, measured on 16 and 64 x 2048 and 1024
-    // x 1024 (one block 14 us, two 23 us); split parts repeat the steps and gates in the first pass (0.17
-    // with the joins).  Many short parts even out the last wave: 16 x 2048 x 1024 takes 2140 us whole,
-    // 1990 in 2 parts, 1740 in 16, but rows that fill the GPU twice are fastest whole.
+    // x 1024 with 16 states in bf16 and used for every shape (one block 14 us, two 23 us); split parts repeat the
+    // steps and gates in the first pass (0.17 with the joins).  Many short parts even out the last wave: in the
+    // form of the kernel that these were measured with, 16 x 2048 x 1024 took 2140 us whole, 1990 in 2 parts and 1740
+    // in 16 (the present one: 1270 in 16), but rows that fill the GPU twice were fastest whole.
     auto chunk_time = [&](long long n) {
         const long long places = (long long)resident * kSMs;
         return n <= places ? 4.7 + 9.2 * ((n + kSMs - 1) / kSMs) : ((double)n / places + 0.35) * (4.7 + 9.2 * resident);
