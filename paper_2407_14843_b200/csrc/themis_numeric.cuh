@@ -152,8 +152,9 @@ constexpr float kExpShift = 1.3e-8f;
 // the lowest A and for -inf too, where 0 times an infinity would be no number.
 __device__ __forceinline__ float log2_rate(float a)
 {
-    const float v = a * kLog2e;
-    return v < -FLT_MAX ? -FLT_MAX : v > FLT_MAX ? FLT_MAX : v;
+    float v = a * kLog2e;
+    asm("max.NaN.f32 %0, %0, %1;\n\tmin.NaN.f32 %0, %0, %2;" : "+f"(v) : "f"(-FLT_MAX), "f"(FLT_MAX));
+    return v;
 }
 __device__ __forceinline__ float decay(float s, float a2) { return ex2(fmaf(s, a2, kExpShift)); }
 __device__ __forceinline__ f32x2 decay2(f32x2 s, f32x2 a2) { return ex2_pair(fma2(s, a2, pack2(kExpShift, kExpShift))); }

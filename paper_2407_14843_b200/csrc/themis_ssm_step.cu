@@ -7,7 +7,7 @@
 // run.  With many rows a thread takes several, so that the parameters are read once for them and
 // several rows' states are on their way at the same time; the values per channel and row (convolution,
 // step, gate) are then computed by one of the channel's lanes each and handed round by shuffles.
-// 16384 rows x 512 channels x 16 states: 254 us, 0.75 of the copy bandwidth (1.24 GB).
+// 16384 rows x 512 channels x 16 states: 227 us, 0.84 of the copy bandwidth (1.24 GB).
 #include <algorithm>
 
 #include "themis_ssm.cuh"
@@ -67,8 +67,6 @@ __device__ __forceinline__ void step_rows(const SsmParams &p, int l, int64_t b0)
     for (int r = 0; r < ROWS; ++r) load4<float, VEC>(h_in + r * h_row, FULL ? 4 : r < rows ? nn : 0, h[r]);
     float A[4];
     load4<float, VEC>(p.in.a + (size_t)dd * N + n0, nn, A);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) A[i] = log2_rate(A[i]);
 
     Pair<T> bq[ROWS][2], cq[ROWS][2];       // B and C of the rows, as they are
     if (VEC) {
@@ -120,6 +118,11 @@ __device__ __forceinline__ void step_rows(const SsmParams &p, int l, int64_t b0)
             }
         }
     }
+
+    // (scaled only here: where A is loaded, the scaling waits for it before the other loads are on their way; 254 us
+    // against 229, 16384 x 512 x 16)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) A[i] = log2_rate(A[i]);
 
     // states; a row that is not on has a step of 0: factors of 1, nothing added
     float v[ROWS];
@@ -211,8 +214,9 @@ template <typename T, int LPC, int ROWS> cudaError_t launch_rows(const SsmParams
 template <typename T, int LPC> cudaError_t launch_lanes(const SsmParams &p, cudaStream_t st)
 {
     // As many rows to a thread as a channel has lanes (up to four: each computes one row's channel values)
-    // once they fill the GPU's threads a few times all the same.  16384 x 512, bf16: 16 states 254 us with
-    // four rows, 283 with two, 455 with one; 8 states 195, 144, 230; 4 states 164, 121, 111.
+    // once they fill the GPU's threads a few times all the same.  16384 x 512, bf16, when all were built: 16 states
+    // 254 us with four rows, 283 with two, 455 with one; 8 states 195, 144, 230; 4 states 164, 121, 111 (the kept ones
+    // are 227, 143 and 111 now).
     const double lanes = (double)p.pr.batch * p.pr.channels * LPC;
     return lanes >= 2.0 * 4 * 2048 * kSMs ? launch_rows<T, LPC, (LPC < 4 ? LPC : 4)>(p, st) : launch_rows<T, LPC, 1>(p, st);
 }
